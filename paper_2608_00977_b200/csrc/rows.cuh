@@ -399,13 +399,15 @@ __device__ __forceinline__ Soft soft_warp(Soft v, float c) {
 //
 // t is one multiply-add, t = c x - (c m) with the rounded product.  The product's rounding error, which is the same
 // for all terms, is known exactly (delta = fma(c, m, -(c m))) and taken out of the sums when the reference moves and at
-// the end, so scores far from zero lose nothing.  Where c m is not far inside fp32 (a row of the type's lowest values),
-// t = c (x - m) in two steps.
+// the end.  Every term carries the factor 2^delta until then, so delta has to stay small: it is at most half a unit of
+// c m, 2^-5 while |c m| < 2^20, but hundreds from |c m| = 2^33 (scores of 1e10 at scale 1), which is beyond fp32's exponents.
+// From 2^20 on, t = c (x - m) in two steps, which has no such term (one instruction more per two elements).
 constexpr float kSlack = 16.f;
+constexpr float kProductMax = 1048576.f;
 template <int N, bool U>
 struct RunningSoft {
   float c, slack, m, delta, high;
-  bool far;          // c m is not far inside fp32
+  bool far;          // |c m| has reached kProductMax: t in two steps
   f32x2 c2, negmc;   // minus the rounded product
   f32x2 s2, u2;
   __device__ __forceinline__ explicit RunningSoft(float scale)
@@ -415,7 +417,7 @@ struct RunningSoft {
   __device__ __forceinline__ void take(const float (&x)[N], float cm) {
     if (cm > high) {
       const float m1 = fmaxf(cm, kLowest), mc = m1 * c;
-      far = !(fabsf(mc) < 1e37f);
+      far = !(fabsf(mc) < kProductMax);
       const float delta1 = far ? 0.f : fmaf(m1, c, -mc);
       const float d = fmaxf(fmaf(m - m1, c, delta1 - delta), kFloor2), f = ex2(d);
       const f32x2 f2 = mk2(f, f);
