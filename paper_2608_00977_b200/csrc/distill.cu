@@ -74,7 +74,7 @@ struct Part {
   Sum rest, listed;
   float W;      // sum of p
   float pl;     // sum of p l
-  float px;     // sum of p (x - listed.m)
+  float px;     // sum of p (x - listed.m) / 2 (halves: see half_diff)
   float bad;    // an id beyond the columns (every CTA sees all ids)
 };
 
@@ -226,8 +226,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
     q.listed.m = warp_max(q.listed.m);
     q.listed.s = q.W = q.pl = q.px = 0.f;
     for (int i = lane; i < k; i += 32) {
-      const float p = p_s[i], d = x_s[i] - q.listed.m;
-      q.listed.s += ex2(max_nan(d * c, kFloor2));
+      const float p = p_s[i], d = half_diff(x_s[i], q.listed.m);
+      q.listed.s += ex2(max_nan(2.f * d * c, kFloor2));
       q.W += p;
       if (p > 0.f || p != p) {
         q.pl += p * l_s[i];
@@ -277,13 +277,13 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
     if (lane == 0) row = {mx, total, W, pT, rest.m, rest.s, rest_f};
     if (part == 0 && a.loss) {
       const float pl = add_warp(o.pl), bad = add_warp(o.bad);
-      const float px = add_warp(o.W == 0.f ? o.px : fmaf(o.W, o.listed.m - listed.m, o.px));
+      const float px = add_warp(o.W == 0.f ? o.px : fmaf(o.W, half_diff(o.listed.m, listed.m), o.px));
       if (lane == 0) {
         // sum p (l - scale (x - mx) + log total)
-        float L = W > 0.f || W != W ? pl - a.scale * fmaf(W, listed.m - mx, px) + W * logf(total) : 0.f;
+        float L = W > 0.f || W != W ? pl - 2.f * a.scale * fmaf(W, half_diff(listed.m, mx), px) + W * logf(total) : 0.f;
         // one logarithm of the ratio keeps a small loss accurate; a tail below fp32's range leaves its reference out of it
         const bool tiny = rest_s <= 1e-30f;
-        if (pT > 0.f) L += pT * (logf(pT * (total / (tiny ? rest.s : rest_s))) - (tiny ? (rest.m - mx) * a.scale : 0.f));
+        if (pT > 0.f) L += pT * (logf(pT * (total / (tiny ? rest.s : rest_s))) - (tiny ? scaled_diff(rest.m, mx, a.scale) : 0.f));
         a.loss[t] = bad != 0.f ? __int_as_float(0x7fffffff) : total == 0.f ? 0.f : L + 0.f * total;
       }
     }

@@ -367,6 +367,11 @@ constexpr float kFloor2 = -200.f;             // 2^-200 is zero in fp32: exponen
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kScaleMin = 1e-20f, kScaleMax = 1e20f;   // accepted scales: c and kFloor2 / c stay far inside fp32
 
+// scale (x - m) of finite scores as far apart as the type allows: the difference is taken in halves, which is exact, so
+// it cannot overflow before a small scale brings it back into range
+__device__ __forceinline__ float half_diff(float x, float m) { return 0.5f * x - 0.5f * m; }
+__device__ __forceinline__ float scaled_diff(float x, float m, float scale) { return half_diff(x, m) * scale * 2.f; }
+
 // ---- running sums of a softmax -------------------------------------------------------------------------------------
 // Of the elements seen so far, with c = scale / log 2 and a reference m:
 //   s = sum 2^t,   u = sum 2^t t,   t = c (x - m).

@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
     if (a.logprob) {
       float lp = 0.f;   // ignored target
       if (y >= a.V || (bad && y >= 0)) lp = nan;
-      else if (y >= 0) lp = xt > -INFINITY ? (xt - ref) * a.scale - log_s : -INFINITY;
+      else if (y >= 0) lp = xt > -INFINITY ? scaled_diff(xt, ref, a.scale) - log_s : -INFINITY;
       a.logprob[t] = lp;
     }
     if (RANK && a.rank) a.rank[t] = count && !bad ? cn : -1;
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
     auto put = [&](int place, uint64_t e) {
       const bool none = e == 0 || bad;
       const float x = order_inv((uint32_t)(e >> 32));
-      a.top_lp[t * k + place] = bad ? nan : none ? -INFINITY : (x - ref) * a.scale - log_s;
+      a.top_lp[t * k + place] = bad ? nan : none ? -INFINITY : scaled_diff(x, ref, a.scale) - log_s;
       a.top_id[t * k + place] = none ? -1 : (int32_t)~(uint32_t)e;
     };
     const uint64_t *from = cand;

@@ -117,3 +117,14 @@ def test_finite_scores_of_any_size(dtype, level, place, n, v):
 def test_scores_at_any_accepted_scale(dtype, scale, n, v):
     g = _gen(v)
     _check_all((torch.randn(n, v, generator=g, device=DEV) * 2).to(dtype), 12, scale, g)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,v", [(6, 3001), (3, 100_003), (460, 2051)])
+def test_the_types_whole_range_at_the_smallest_scale(dtype, n, v):
+    """Scores further apart than the type's largest value, which the scale brings back."""
+    g = _gen(1)
+    x = (torch.rand(n, v, generator=g, device=DEV) * 2 - 1) * 3.0e38
+    x[1] = torch.finfo(dtype).min
+    x[2, :2000] = torch.finfo(dtype).min
+    _check_all(x.to(dtype), 8, 1e-20, g)
