@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
   // ---- first pass: the sum over the columns outside the list
   const f32x2 c2 = mk2(c, c);
   RunningSoft<n, false> sums(a.scale);
+  float top = -INFINITY;   // its largest
   // calls f(i, j, u) for the listed columns of pair p: place i of the list, element u of the pair's chunk j
   auto listed_of = [&](int32_t p, auto f) {
 #pragma unroll 1
@@ -194,6 +195,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
     float x[n];
     unpack<T, 8>(raw, x);
     const float cm = fmaxf(chunk_max<T>(raw[0], raw[1], raw[2], raw[3]), chunk_max<T>(raw[4], raw[5], raw[6], raw[7]));
+    top = fmaxf(top, cm);
     sums.take(x, cm);
   };
   // the listed columns are struck out of the staged pair before it is read
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
     x_s[tid] = counts ? my_x : -INFINITY;
   }
   {
-    const Soft part_sum = sums.result();
+    const Soft part_sum = sums.result(top);
     Sum v = {part_sum.m, part_sum.s};
     v = sum_warp(v, c);
     if (lane == 0) sh_sum[w] = v;

@@ -453,17 +453,26 @@ struct RunningSoft {
     s2 = add2(s2, e);
     if (U) u2 = fma2(e, mk2(t0, t1), u2);
   }
-  __device__ __forceinline__ Soft result() const {
-    float a, b;
+  // The sums about `top`, the largest of the elements (minus infinity: there were none).  Dividing by its own term, as
+  // the pass formed it, leaves exactly 1 of it and takes delta out of the others, so s >= 1 and a row with nearly all its
+  // mass in one column keeps what the others add.
+  __device__ __forceinline__ Soft result(float top) const {
+    float a, b, tm;
     Soft r;
     un2(s2, a, b);
-    const float f = ex2(-delta), s = a + b;
-    r.m = m;
-    r.s = s * f;
+    r.m = kLowest;
+    r.s = a + b;
     r.u = 0.f;
-    if (U) {
-      un2(u2, a, b);
-      r.u = f * fmaf(-delta, s, a + b);
+    if (top > -INFINITY) {
+      un2(negmc, tm, tm);
+      tm = far ? (top - m) * c : fmaf(top, c, tm);
+      const float e = ex2(tm), s = r.s;
+      r.m = top;
+      r.s = s / e;
+      if (U) {
+        un2(u2, a, b);
+        r.u = fmaf(-tm, s, a + b) / e;
+      }
     }
     return r;
   }

@@ -170,7 +170,6 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
   int32_t *const sel = sm.top.sel;
   // written by the other CTAs of the cluster into its first CTA
   __shared__ Soft all_soft[kRowClusterMax];
-  __shared__ uint32_t all_max[kRowClusterMax];   // maxima, as shifted orders
   __shared__ int32_t all_cnt[kRowClusterMax];
 
   const RowChunks<T> r(static_cast<const T *>(a.x) + t * a.stride, a.V);
@@ -239,7 +238,7 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
   stream.run(take);
 
   // ---- join: thread -> warp -> CTA
-  Soft v = sums.result();
+  Soft v = sums.result(mk);
   float ahead = 0.f;   // up to 2^31 columns: a thread's count is exact in fp32, the joins add whole numbers
   if (RANK) {
     float a_0, a_1;
@@ -268,13 +267,11 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
     q.s = q.u = 0.f;
     if (lane < NW) q = sh_soft[lane];
     q = soft_warp(q, c);
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, lane < NW ? sh_hi[lane] : 0u);
     int32_t cn = RANK && lane < NW ? __float_as_int(sh_cnt[lane]) : 0;
     cn = __reduce_add_sync(0xffffffffu, cn);
     if (lane == 0) {
       *(S > 1 ? cluster.map_shared_rank(&all_soft[part], 0) : &all_soft[0]) = q;
       *(S > 1 ? cluster.map_shared_rank(&all_cnt[part], 0) : &all_cnt[0]) = cn;
-      *(S > 1 ? cluster.map_shared_rank(&all_max[part], 0) : &all_max[0]) = hi;
     }
   }
 
@@ -416,7 +413,6 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
   // ---- the row's results
   Soft tot = all_soft[0];
   int32_t cn = all_cnt[0];
-  uint32_t top = all_max[0];
   if (S > 1) {   // lane q: CTA q's part
     const bool in = lane < S;
     tot.m = in ? all_soft[lane].m : kLowest;
@@ -424,25 +420,21 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
     tot.u = in ? all_soft[lane].u : 0.f;
     tot = soft_warp(tot, c);
     cn = __reduce_add_sync(0xffffffffu, in ? all_cnt[lane] : 0);
-    top = __reduce_max_sync(0xffffffffu, in ? all_max[lane] : 0u);
   }
   const bool bad = !(tot.s <= 3.0e38f);   // NaN or plus infinity in the row
   const bool empty = tot.s == 0.f;        // no finite element
   const float nan = __int_as_float(0x7fffffff);
-  const float log_s = bad ? nan : empty ? -INFINITY : logf(tot.s);   // about the reference
-  const float ref = bad ? nan : empty ? -INFINITY : tot.m;
+  const float log_s = bad ? nan : empty ? -INFINITY : logf(tot.s);   // s >= 1
+  const float row_max = bad ? nan : empty ? -INFINITY : tot.m;
   if (tid == 0) {
-    // the maximum itself, from its order: the dropped low bits are zeros, or ones below zero
-    uint32_t o = top << El<T>::kShift;
-    if (El<T>::kShift > 0 && !(o >> 31)) o |= (1u << El<T>::kShift) - 1u;
-    const float row_max = bad || empty ? ref : order_inv(o);
     if (a.row_max) a.row_max[t] = row_max;
-    if (a.log_sum) a.log_sum[t] = bad || empty ? log_s : fmaf(ref - row_max, a.scale, log_s);
-    if (a.entropy) a.entropy[t] = bad ? nan : empty ? 0.f : log_s - kLn2 * (tot.u / tot.s);
+    if (a.log_sum) a.log_sum[t] = log_s;
+    // u is below zero but for its rounding
+    if (a.entropy) a.entropy[t] = bad ? nan : empty ? 0.f : log_s - kLn2 * (fminf(tot.u, 0.f) / tot.s);
     if (a.logprob) {
       float lp = 0.f;   // ignored target
       if (y >= a.V || (bad && y >= 0)) lp = nan;
-      else if (y >= 0) lp = xt > -INFINITY ? scaled_diff(xt, ref, a.scale) - log_s : -INFINITY;
+      else if (y >= 0) lp = xt > -INFINITY ? scaled_diff(xt, row_max, a.scale) - log_s : -INFINITY;
       a.logprob[t] = lp;
     }
     if (RANK && a.rank) a.rank[t] = count && !bad ? cn : -1;
@@ -451,7 +443,7 @@ __global__ void __launch_bounds__(NT, 896 / NT) token_logprobs_kernel(const LpAr
     auto put = [&](int place, uint64_t e) {
       const bool none = e == 0 || bad;
       const float x = order_inv((uint32_t)(e >> 32));
-      a.top_lp[t * k + place] = bad ? nan : none ? -INFINITY : scaled_diff(x, ref, a.scale) - log_s;
+      a.top_lp[t * k + place] = bad ? nan : none ? -INFINITY : scaled_diff(x, row_max, a.scale) - log_s;
       a.top_id[t * k + place] = none ? -1 : (int32_t)~(uint32_t)e;
     };
     const uint64_t *from = cand;
