@@ -415,7 +415,8 @@ enum { TSID_TOP_MAX = 128 }; /* longest list of best columns */
 /* Lookup with scaling: out[t, :] = scale * table[ids[t], :] for t < n_tokens, dim elements a row.
  * ids are int32 (ids_i64 = 0) or int64 (1).  A token whose id is pad_id gives a zero row.  An id outside
  * [0, n_rows) that is not pad_id gives a row of NaN and sets *d_flag_or_null (DEVICE int32, never cleared here)
- * to 1.  table and out may have different types. */
+ * to 1.  table and out may have different types.
+ * dim <= 2^31 - 1024. */
 tsid_status_t tsid_embed(int64_t n_tokens, int32_t n_rows, int32_t dim, const void *d_table, int32_t table_dtype,
                          int64_t table_stride, const void *d_ids, int32_t ids_i64, int64_t pad_id, float scale,
                          void *d_out, int32_t out_dtype, int64_t out_stride, int32_t *d_flag_or_null, void *stream);

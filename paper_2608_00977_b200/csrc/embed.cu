@@ -41,6 +41,8 @@ __device__ __forceinline__ int64_t load_id(const void *ids, int64_t t, int is64)
 struct Slice {
   int e, cs, dim;   // first element, distance to the next, row length
 };
+// Indices are 32-bit and run past the row's end by less than the elements of one step of a group, 32 lanes x 8.
+constexpr int32_t kRowMax = 2147483647 - 1023;
 template <typename T, int VE, bool WIDE>
 struct Elems {
   static constexpr int kWords = WIDE ? VE * (int)sizeof(T) / 4 : VE;
@@ -997,6 +999,7 @@ tsid_status_t tsid_embed(int64_t n_tokens, int32_t n_rows, int32_t dim, const vo
                          int64_t table_stride, const void *d_ids, int32_t ids_i64, int64_t pad_id, float scale,
                          void *d_out, int32_t out_dtype, int64_t out_stride, int32_t *d_flag_or_null, void *stream) {
   if (n_tokens < 0 || n_rows < 1 || dim < 1) return refuse(TSID_ERR_INVALID_ARG, "n_tokens must be >= 0, n_rows and dim >= 1");
+  if (dim > kRowMax) return refuse(TSID_ERR_UNSUPPORTED, "dim above 2^31 - 1024");
   if (!dtype_ok(table_dtype) || !dtype_ok(out_dtype)) return refuse(TSID_ERR_INVALID_ARG, "bad dtype");
   if (n_tokens == 0) return TSID_OK;
   if (n_tokens > 2147483647LL) return refuse(TSID_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens");

@@ -1,0 +1,23 @@
+"""Operators on factor rows and score rows without a GPU: sizes at the limits of the interface are refused before any
+CUDA call, or reported as documented."""
+import ctypes as C
+
+import pytest
+
+from paper_2608_00977_b200 import binding as B
+
+P = 1 << 20      # an address that is never read: the calls below are refused first
+
+
+@pytest.fixture(scope="module")
+def L():
+    import __graft_entry__ as g
+    g.build()
+    return B.lib()
+
+
+@pytest.mark.parametrize("dim", [2 ** 31 - 1, 2 ** 31 - 8, 2 ** 31 - 512, 2 ** 31 - 1023])
+def test_lookup_refuses_rows_whose_indices_would_leave_32_bits(L, dim):
+    assert L.tsid_embed(4, 10, dim, P, 1, dim, P, 0, -1, 1.0, P, 1, dim, None, None) == B.TSID_ERR_UNSUPPORTED
+    assert b"dim" in L.tsid_last_error(None)
+    assert L.tsid_embed(0, 10, 2 ** 31 - 1024, None, 1, 0, None, 0, -1, 1.0, None, 1, 0, None, None) == B.TSID_OK
