@@ -508,6 +508,15 @@ def _raise_last(st):
     raise TsidError(st, lib().tsid_last_error(None).decode())
 
 
+_INT_MAX = 2 ** 31 - 1   # of the interface's 32-bit sizes; ctypes would cut larger numbers off
+
+
+def _size32(n, name):
+    if not -_INT_MAX <= n <= _INT_MAX:
+        raise ValueError("%s must be below 2^31" % name)
+    return n
+
+
 def _rows_of(t, name, device=None):
     """A matrix argument: (rows, columns, row stride, tsid_dtype_t)."""
     dt = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
@@ -517,6 +526,8 @@ def _rows_of(t, name, device=None):
     s, e = t.stride()
     if m < 1 or (e != 1 and m > 1) or (s < m and n > 1):
         raise ValueError("%s must have rows of at least one element, contiguous within a row" % name)
+    if m > _INT_MAX:
+        raise ValueError("%s must have fewer than 2^31 columns" % name)
     if device is not None and t.device != device:
         raise ValueError("%s must be on %s" % (name, device))
     return n, m, s, dt
@@ -575,6 +586,7 @@ def tsid_embed(table, ids, scale=1.0, pad_id=-1, out=None, out_dtype=None, flag=
     zero row.  Returns out, [number of ids, dim], of the table's type unless out or out_dtype says otherwise.  An id
     outside the table gives a NaN row and sets `flag` (CUDA int32 tensor with one element) if given."""
     n_rows, dim, tstride, tdt = _rows_of(table, "table")
+    _size32(n_rows, "the table's number of rows")
     dev = table.device
     ids_ptr, i64 = _ids_of(ids, "ids", dev)
     n = ids.numel()
@@ -595,7 +607,7 @@ def tsid_embed(table, ids, scale=1.0, pad_id=-1, out=None, out_dtype=None, flag=
 
 def tsid_embed_grad_workspace_bytes(n_tokens, n_rows, dim) -> int:
     need = C.c_size_t(0)
-    st = lib().tsid_embed_grad_workspace_bytes(n_tokens, n_rows, dim, C.byref(need))
+    st = lib().tsid_embed_grad_workspace_bytes(n_tokens, _size32(n_rows, "n_rows"), _size32(dim, "dim"), C.byref(need))
     if st != TSID_OK:
         _raise_last(st)
     return need.value
@@ -607,6 +619,7 @@ def tsid_embed_grad(grad_out, ids, n_rows, scale=1.0, pad_id=-1, out=None, out_d
     dim], fp32 unless out or out_dtype says otherwise; with accumulate=True it is added to `out`.  `workspace`: a
     CUDA uint8 tensor of at least tsid_embed_grad_workspace_bytes(...) + 256 bytes (allocated here if not given)."""
     n, dim, ystride, ydt = _rows_of(grad_out, "grad_out")
+    _size32(n_rows, "n_rows")
     dev = grad_out.device
     ids_ptr, i64 = _ids_of(ids, "ids", dev, n)
     if accumulate and out is None:

@@ -21,3 +21,10 @@ def test_lookup_refuses_rows_whose_indices_would_leave_32_bits(L, dim):
     assert L.tsid_embed(4, 10, dim, P, 1, dim, P, 0, -1, 1.0, P, 1, dim, None, None) == B.TSID_ERR_UNSUPPORTED
     assert b"dim" in L.tsid_last_error(None)
     assert L.tsid_embed(0, 10, 2 ** 31 - 1024, None, 1, 0, None, 0, -1, 1.0, None, 1, 0, None, None) == B.TSID_OK
+
+
+@pytest.mark.parametrize("rows,dim", [(2 ** 32 + 10, 8), (2 ** 31, 8), (10, 2 ** 32 + 8), (-2 ** 32 + 5, 8)])
+def test_sizes_beyond_the_interface_are_not_cut_to_32_bits(L, rows, dim):
+    """(2^32 + 10 rows were taken for 10.)"""
+    with pytest.raises(ValueError, match="2\\^31"):
+        B.tsid_embed_grad_workspace_bytes(1000, rows, dim)
