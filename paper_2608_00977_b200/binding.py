@@ -721,7 +721,7 @@ def tsid_distill(logits, teacher_id, teacher_logprob, mode=TSID_DISTILL_TAIL, sc
     sum(weight * loss) in the same launch."""
     n, v, stride, dt = _rows_of(logits, "logits")
     dev = logits.device
-    if teacher_id.dim() != 2 or teacher_id.shape[0] != n:
+    if not isinstance(teacher_id, torch.Tensor) or teacher_id.dim() != 2 or teacher_id.shape[0] != n:
         raise ValueError("teacher_id must be [%d, top_k]" % n)
     k = teacher_id.shape[1]
     ip = _vector(teacher_id, torch.int32, n * k, "teacher_id", dev)

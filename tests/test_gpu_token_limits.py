@@ -1,4 +1,4 @@
-"""Operators on factor rows and score rows: matrices with more rows or columns than the interface counts."""
+"""Operators on factor rows and score rows: arguments that the Python layer refuses before the call."""
 import pytest
 import torch
 
@@ -23,3 +23,10 @@ def test_matrices_beyond_the_interface_are_refused():
                  lambda: B.tsid_distill(scores, listed, one.view(1, 1))):
         with pytest.raises(ValueError, match="2\\^31"):
             call()
+
+
+def test_a_list_that_is_not_a_tensor_is_refused():
+    x = torch.zeros(2, 5, device=DEV)
+    for ids, lp in ((None, None), ([[0], [1]], x[:, :1].contiguous()), (torch.zeros(2, 1, dtype=torch.int32, device=DEV), None)):
+        with pytest.raises(ValueError):
+            B.tsid_distill(x, ids, lp)
