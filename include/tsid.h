@@ -408,7 +408,9 @@ const char *tsid_last_error(const tsid_template_t *t);
  * (cudaStream_t, 0 = legacy default stream), never synchronise and allocate nothing; messages via
  * tsid_last_error(NULL).  Matrices are row-major with a row stride in ELEMENTS (>= the row length) and need no
  * alignment beyond their element's.  Sums, softmax statistics and per-row results are fp32; a 16-bit output is
- * rounded once, to nearest even.  Zero rows or tokens are fine.  Identical inputs give bitwise identical outputs. */
+ * rounded once, to nearest even.  Zero rows or tokens are fine.  Identical inputs give bitwise identical outputs where
+ * types, strides and the addresses modulo 16 bytes are the same too: rows are cut at 16-byte boundaries and moved by the
+ * widest accesses that fit, so another layout may add the same terms in another order. */
 typedef enum { TSID_DT_F32 = 0, TSID_DT_BF16 = 1, TSID_DT_F16 = 2 } tsid_dtype_t;
 enum { TSID_TOP_MAX = 128 }; /* longest list of best columns */
 
@@ -424,7 +426,8 @@ tsid_status_t tsid_embed(int64_t n_tokens, int32_t n_rows, int32_t dim, const vo
 /* Its gradient by sorted ids: grad_table[v, :] = scale * sum over t with ids[t] = v of grad_out[t, :], plus the
  * old grad_table[v, :] when accumulate is 1 (rows whose id does not occur are then left alone, otherwise they
  * become zero).  Padding and ids outside the table contribute nothing; the latter set the flag.  The sums run in
- * fp32 in an order that depends on the sizes only (no float atomics).  grad_table must not overlap grad_out.
+ * fp32 in an order that depends on the ids, the sizes, the types and the layout only (no float atomics).  grad_table
+ * must not overlap grad_out.
  * workspace: DEVICE, 256-byte aligned, tsid_embed_grad_workspace_bytes(...) bytes, free again when the work
  * enqueued here is done; a batch of up to 256 tokens needs none (0 bytes, workspace may be NULL).  dim <= 2^20. */
 tsid_status_t tsid_embed_grad_workspace_bytes(int64_t n_tokens, int32_t n_rows, int32_t dim, size_t *h_bytes_out);
