@@ -429,7 +429,8 @@ tsid_status_t tsid_embed(int64_t n_tokens, int32_t n_rows, int32_t dim, const vo
  * fp32 in an order that depends on the ids, the sizes, the types and the layout only (no float atomics).  grad_table
  * must not overlap grad_out.
  * workspace: DEVICE, 256-byte aligned, tsid_embed_grad_workspace_bytes(...) bytes, free again when the work
- * enqueued here is done; a batch of up to 256 tokens needs none (0 bytes, workspace may be NULL).  dim <= 2^20. */
+ * enqueued here is done; a batch of up to 256 tokens on a table of fewer than 2^24 rows needs none (0 bytes, workspace
+ * may be NULL).  dim <= 2^20. */
 tsid_status_t tsid_embed_grad_workspace_bytes(int64_t n_tokens, int32_t n_rows, int32_t dim, size_t *h_bytes_out);
 tsid_status_t tsid_embed_grad(int64_t n_tokens, int32_t n_rows, int32_t dim, const void *d_grad_out,
                               int32_t grad_out_dtype, int64_t grad_out_stride, const void *d_ids, int32_t ids_i64,

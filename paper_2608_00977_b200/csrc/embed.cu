@@ -289,9 +289,9 @@ __device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t *sh) { 
 // ---- sort of up to 16 x 4096 tokens: one cluster, the items in its shared memory -----------------------------------
 // Each CTA of the first cluster keeps its share of the items in registers; a pass ranks them (warp ballots, digit
 // counters per warp, digit totals exchanged through distributed shared memory) and stores each to its place in the
-// owning CTA's shared memory, the last pass to global memory.  The digit has up to 9 bits, so tables of 2^18 rows
-// take two passes.  Sorting on 16 SMs leaves the others idle, so the launch's other clusters zero the whole table (the rows
-// that occur are written again by the sums).
+// owning CTA's shared memory, the last pass to global memory.  The digit has up to 9 bits, so tables of fewer than
+// 2^18 rows take two passes (the number of rows is itself a key).  Sorting on 16 SMs leaves the others idle, so the
+// launch's other clusters zero the whole table (the rows that occur are written again by the sums).
 constexpr int CS_THREADS = 1024, CS_WARPS = CS_THREADS / 32, CS_RADIX = 512;
 template <int ITEMS>
 constexpr size_t cs_smem() {

@@ -1,7 +1,5 @@
 """Operators on factor rows and score rows without a GPU: sizes at the limits of the interface are refused before any
 CUDA call, or reported as documented."""
-import ctypes as C
-
 import pytest
 
 from paper_2608_00977_b200 import binding as B
@@ -28,3 +26,13 @@ def test_sizes_beyond_the_interface_are_not_cut_to_32_bits(L, rows, dim):
     """(2^32 + 10 rows were taken for 10.)"""
     with pytest.raises(ValueError, match="2\\^31"):
         B.tsid_embed_grad_workspace_bytes(1000, rows, dim)
+
+
+def test_a_small_batch_needs_no_workspace_below_2_24_rows(L):
+    """256 tokens fit one launch while a row number and a token's place fit one word."""
+    for tokens, rows, none in ((256, 2 ** 24 - 1, True), (256, 2 ** 24, False), (257, 2 ** 24 - 1, False), (1, 2 ** 24, False),
+                               (0, 10, True)):
+        need = B.tsid_embed_grad_workspace_bytes(tokens, rows, 8)
+        assert (need == 0) == none, (tokens, rows, need)
+    assert L.tsid_embed_grad(256, 2 ** 24, 8, P, 0, 8, P, 0, -1, 1.0, P, 0, 8, 0, None, 0, None, None) == B.TSID_ERR_INVALID_ARG
+    assert b"workspace" in L.tsid_last_error(None)
