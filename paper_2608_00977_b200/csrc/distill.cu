@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
   const int64_t t = (int64_t)blockIdx.x / S;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
 
-  // the listed columns in this CTA's part (id -1: empty place, or elsewhere): log probability, probability, score, and
-  // what stands in for the score (first pass) and becomes the gradient (second pass)
+  // the listed columns in this CTA's part (id -1: empty place, or elsewhere): log probability, probability, score and
+  // gradient
   __shared__ int32_t id_s[kListMax], next_s[kListMax];
   __shared__ float l_s[kListMax], p_s[kListMax], x_s[kListMax], v_s[kListMax];
   __shared__ __align__(8) uint32_t mark[kMarkWords];
@@ -132,7 +132,6 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const DistillArg
     if (my_id >= a.V) beyond = 1;
     id_s[tid] = own ? my_id : -1;
     l_s[tid] = my_id >= 0 && my_id < a.V ? my_l : -INFINITY;
-    v_s[tid] = -INFINITY;
     if (own) next_s[tid] = atomicExch(&head[my_word], tid);
   }
   __syncthreads();
