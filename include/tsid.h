@@ -410,7 +410,9 @@ const char *tsid_last_error(const tsid_template_t *t);
  * alignment beyond their element's.  Sums, softmax statistics and per-row results are fp32; a 16-bit output is
  * rounded once, to nearest even.  Zero rows or tokens are fine.  Identical inputs give bitwise identical outputs where
  * types, strides and the addresses modulo 16 bytes are the same too: rows are cut at 16-byte boundaries and moved by the
- * widest accesses that fit, so another layout may add the same terms in another order. */
+ * widest accesses that fit, so another layout may add the same terms in another order.  Exponentials are the
+ * hardware's 2^x (two units in the last place; below 2^-126 they are zero).  Where few rows are long, and in the sort of a
+ * gradient, one cluster of up to 16 CTAs works on them: a device partition that cannot hold it gives TSID_ERR_CUDA. */
 typedef enum { TSID_DT_F32 = 0, TSID_DT_BF16 = 1, TSID_DT_F16 = 2 } tsid_dtype_t;
 enum { TSID_TOP_MAX = 128 }; /* longest list of best columns */
 
@@ -479,7 +481,8 @@ tsid_status_t tsid_token_logprobs_grad(int64_t n_rows, int32_t n_cols, const voi
  * grad is the gradient of sum_t weight[t] loss[t] (weight NULL: 1) with respect to the logits; loss itself is not
  * weighted.  Loss, gradient, or both; one read of the logits from memory and one write of the gradient.  A row
  * whose student logits are all -inf has loss 0 and gradient 0.  An id >= n_cols makes the row's loss NaN and is
- * otherwise skipped; of a repeated id the first place counts.  grad: type, stride and aliasing as above.
+ * otherwise skipped; of a repeated id the first place counts.  grad: type, stride and aliasing as above; before a 16-bit
+ * gradient is rounded it may be off by 2^-16 of itself (its exponent is formed in one step).
  * 1 <= top_k <= TSID_TOP_MAX (places, which may outnumber the columns). */
 typedef enum { TSID_DISTILL_RENORM = 0, TSID_DISTILL_TAIL = 1 } tsid_distill_mode_t;
 tsid_status_t tsid_distill(int64_t n_rows, int32_t n_cols, const void *d_logits, int32_t logits_dtype,

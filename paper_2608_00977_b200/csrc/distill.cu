@@ -14,11 +14,14 @@
 // tail keeps its accuracy; a warp finds the few chunks that hold a listed column with one bit per 16-byte chunk, by its
 // number modulo 32 kMarkWords, in shared memory.
 //
-// What bounds it: 2048 x 100,000 bf16 with 64 listed columns takes 196 us against 125 us for one read and one write at
-// the copy rate (6.55 TB/s).  DRAM traffic is that minimum (428 MB read, the gradient written), but two 2^x and some 18
-// instructions per element keep the SMs busy (issue slots 58 %, the 2^x unit 50 %), and a CTA's two passes cannot
-// overlap.  Tried and slower: the row held in shared memory between the passes by clusters of 4 to 8 CTAs (258 - 310 us:
-// short CTAs, whose set-up and cluster barriers outweigh the saved L2 reads), one CTA of 512 threads a row (201 us).
+// What bounds it (times of the kernel alone; a call in a sequence of calls takes 2 to 12 us more): 2048 x 100,000 bf16 with 64
+// listed columns takes 197 us against 125 us for one read and one write at the copy rate (6.55 TB/s), the loss alone 103 us.
+// DRAM traffic is that minimum (428 MB read, the gradient written).  No unit is full: issue slots 58 %, the 2^x unit 50 %
+// (two 2^x and some 18 instructions per element), memory 64 %, 44 % of the warps active; a CTA's two passes follow each other
+// with a join between them, in which it loads nothing.  The time is linear in the rows (1960 to 2400 rows: 0.096 us each, no
+// step at a whole wave).  How far the student is makes 1 %.  Tried and slower: the row held in shared memory
+// between the passes by clusters of 4 to 8 CTAs (258 - 310 us: short CTAs, whose set-up and cluster barriers outweigh the
+// saved L2 reads), one CTA of 512 threads a row (201 us).
 #include <cooperative_groups.h>
 
 #include <algorithm>

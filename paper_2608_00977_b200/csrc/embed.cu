@@ -12,10 +12,13 @@
 // access that the rows' alignment allows): no float atomics, the same call gives the same bits, and a popular id is
 // spread over as many groups as it has places.
 //
-// Measured on one B200 (6.55 TB/s copy rate).  Lookup of 1M x 128 bf16: 83 us, 6.2 TB/s (95 %).  Gradient: 1M tokens x
-// 128 bf16 into a table of 1M rows fp32 185 us (118 us for one read and one write): 50 us of sorting, which is latency,
-// 125 us of sums and zeroing at 6.2 TB/s, 10 us of joining.  65,536 x 64 bf16, 100,000 rows: 32 us (5.3), nearly all
-// latency of the sort (17 us), the sums (8) and the join (4).  129 x 33 fp32, 2,000 rows: 6.3 us in one launch.
+// Measured on one B200 (6.55 TB/s copy rate; times of the kernels alone, a call in a sequence of calls takes 1 to 10 us more).
+// Lookup of 1M x 128 bf16: 83 us, 6.2 TB/s (95 %); rows that are no multiple of 8 bytes go element by element and are bound by
+// instructions (1M x 125 bf16 255 us, fp32 204).  Gradient: 1M tokens x 128 bf16 into a table of 1M rows fp32 188 us (118 us
+// for one read and one write): 50 us of sorting, in which memory idles, 125 us of sums and zeroing at 6.2 TB/s, 10 us of
+// joining; accumulating costs the read of the named rows (with ids spread evenly 237 us, overwriting 184).  65,536 x 64 bf16,
+// 100,000 rows: 33 us (5.3), nearly all latency of the sort (17 us), the sums (8) and the join (4).  129 x 33 fp32, 2,000
+// rows: 6.2 us in one launch.
 #include <cooperative_groups.h>
 
 #include <algorithm>

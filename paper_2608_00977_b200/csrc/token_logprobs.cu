@@ -15,11 +15,15 @@
 // of them, and their elements at or above the bound are ranked by counting.  All comparisons are on (value, index)
 // pairs, which are distinct, so ties need no special case and constant rows cost no more than others.
 //
-// What bounds it (one B200, 6.55 TB/s copy rate): with 16-bit scores the instructions and the 2^x unit, not memory: per
-// element one 2^x (the unit gives 16 per clock and SM, 45 us for 2048 x 100,000) and about 8 other instructions, with
-// lists and rank about 11.  2048 x 100,000 bf16 without lists 74 us (62.6 us at the copy rate), 64 x 1,000,000 bf16 with
-// rank and 50 best 47 us (19.6), 4096 x 20,000 fp32 with rank and 10 best 75 us (50.1).  One row is latency: 100,000
-// columns with 20 best 11.4 us, of which the pass takes 5.
+// What bounds it (one B200, 6.55 TB/s copy rate; times are of the kernel alone, a call in a sequence of calls takes 2 to 7 us
+// more).  Per element one 2^x (the unit gives 16 per clock and SM) and about 8 other instructions, with lists and rank about
+// 11, with fp32 scores 21.  Many rows without lists come near the copy rate: 2048 x 100,000 bf16 76 us (62.6 for its bytes),
+// 4096 x 20,000 fp32 55 us (50.1); with rank 62, with 10 best 68, with both 76 us, where issue slots are 66 % busy and a row's end
+// takes a quarter of its time.  Few long rows fill no unit (64 x 1,000,000 bf16 with rank and 50 best: 47 us against 19.6 for its
+// bytes, issue slots 58 % busy, the 2^x unit 36 %, memory 40 %): the statistics alone take 32 us, the rank and the list 7 to 8
+// us each, and the time goes in steps by how clusters fit on the chip (47 us for 37 rows of 12 CTAs and for 64 of 6, 66 us
+// for 74 of 6).
+// One row is latency: 100,000 columns with 20 best 11.7 us, of which the pass takes 5.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -493,10 +497,10 @@ cudaError_t launch_lp(const LpArgs &a, int64_t rows, int S, cudaStream_t st) {
 }
 
 // CTAs per row and their size.  Few rows: 256 threads and as many CTAs per row as fill three to an SM (64 rows of
-// 1,000,000 bf16, rank and 50 best: 46 us with 6 CTAs, 60 with 8, with 16 of 128 threads 59), as long as a CTA keeps 32 KB
+// 1,000,000 bf16, rank and 50 best: 47 us with 6 CTAs, 60 with 8, with 16 of 128 threads 59), as long as a CTA keeps 32 KB
 // of the row, since joining the lists costs 2 to 3 us (200 rows of 5,000 fp32: 8.2 us with one CTA, 9.8 with two; one row
 // of 100,000 bf16: 11.4 with 6, 11.5 with 16).  Many rows: one CTA of 128 threads each, of which seven share an SM, so that
-// the end of one row, which is latency, hides behind the passes of six others (4096 rows of 20,000 fp32: 74 us, with
+// the end of one row, which is latency, hides behind the passes of six others (4096 rows of 20,000 fp32: 76 us, with
 // 256 threads 108 us).
 template <typename T>
 cudaError_t dispatch_lp(const LpArgs &a, int64_t rows, cudaStream_t st) {
